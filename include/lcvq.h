@@ -471,13 +471,13 @@ lcvq_status_t lcvq_attn_paged(int64_t T, int32_t B, int32_t Hq, int32_t Hkv, int
 size_t lcvq_attn_workspace_bytes(int64_t T, int32_t B, int32_t Hq, int32_t Hkv, int32_t D, int32_t max_q);
 
 /*
- * lcvq_linear_fwd_int4 -- the layer output from 4-bit weights with a scale per row and
+ * lcvq_linear_fwd_int4 -- the layer output from 4-bit weights with a scale s per row and
  * group of columns, for layers that are not LC-VQ (an output head, say):
- *   Y[t, r] = sum_k scales[k, r] sum_{c in group k} (code[r, c] - z[k, r]) X[t, c]
+ *   Y[t, r] = sum_k s[r, k] sum_{c in group k} (code[r, c] - z[r, k]) X[t, c]
  *   packed   m x n / 2 bytes, code[r, c] (0..15) in the low half of byte r n/2 + c/2 for
  *            even c, the high half for odd c
- *   scales   n / group x m bf16: one row of m per group of columns
- *   zeros    n / group x m bf16 (any value, whole or not), or NULL for 8 everywhere
+ *   scales   bf16: n / group x m, one row of m per group of columns
+ *   zeros    bf16 (any value, whole or not), in the order of scales, or NULL for 8 everywhere
  *   X        N x n bf16;  Y  N x m, y_dtype BF16 or F32
  * group is 32, 64 or a multiple of 128 and divides n; m >= 0 is any number.  Sums are
  * fp32, the codes in them as 16 + code and taken back by each group's sum of X: a token with
@@ -492,6 +492,17 @@ lcvq_status_t lcvq_linear_fwd_int4(int64_t N, int64_t m, int64_t n, int32_t grou
                                    const void *scales, const void *zeros, const void *X, void *Y, int32_t y_dtype,
                                    void *workspace, size_t workspace_bytes, void *stream);
 size_t lcvq_int4_workspace_bytes(int64_t N, int64_t m, int64_t n);
+
+/*
+ * lcvq_linear_fwd_int4_ex -- lcvq_linear_fwd_int4 with scales and zeros in either order:
+ *   LCVQ_SCALES_BY_GROUP  n / group x m, as there
+ *   LCVQ_SCALES_BY_ROW    m x n / group: one row of n / group per weight row
+ * All other arguments, the workspace and the bits of Y are the same.
+ */
+typedef enum { LCVQ_SCALES_BY_GROUP = 0, LCVQ_SCALES_BY_ROW = 1 } lcvq_scales_order_t;
+lcvq_status_t lcvq_linear_fwd_int4_ex(int64_t N, int64_t m, int64_t n, int32_t group, const uint8_t *packed,
+                                      const void *scales, const void *zeros, int32_t scales_order, const void *X,
+                                      void *Y, int32_t y_dtype, void *workspace, size_t workspace_bytes, void *stream);
 
 /*
  * Instrumentation: device time of individual kernels, measured with HIP events.

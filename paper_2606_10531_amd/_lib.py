@@ -19,6 +19,8 @@ OP_FWD, OP_BWD, OP_FWD_PACKED = 0, 1, 2
 EST_STE, EST_DGE = 0, 1
 # lcvq_kv_format_t
 KV_E4M3, KV_BF16 = 0, 1
+# lcvq_scales_order_t
+SCALES_BY_GROUP, SCALES_BY_ROW = 0, 1
 # lcvq_kernel_t
 KERNELS = ["fwd_prep", "fwd", "bwd_prep", "dx", "dw", "pack", "dequant", "fill", "adam", "packed_prep",
            "packed", "encode", "map_sum", "kv_write", "kv_read", "attn_few", "attn_wide",
@@ -64,6 +66,7 @@ SIGNATURES = {
                                _P, _I32, ctypes.c_float, _I32, _I32, _P, _P, _P, _SZ, _P]),
     "lcvq_attn_workspace_bytes": (_SZ, [_I64, _I32, _I32, _I32, _I32, _I32]),
     "lcvq_linear_fwd_int4": (_I32, [_I64, _I64, _I64, _I32, _P, _P, _P, _P, _P, _I32, _P, _SZ, _P]),
+    "lcvq_linear_fwd_int4_ex": (_I32, [_I64, _I64, _I64, _I32, _P, _P, _P, _I32, _P, _P, _I32, _P, _SZ, _P]),
     "lcvq_int4_workspace_bytes": (_SZ, [_I64, _I64, _I64]),
     "lcvq_timer_enable": (_I32, [ctypes.c_uint32]),
     "lcvq_timer_read": (_I32, [_I32, ctypes.POINTER(ctypes.c_double), ctypes.POINTER(ctypes.c_int64)]),

@@ -1014,6 +1014,13 @@ size_t lcvq_int4_workspace_bytes(int64_t N, int64_t m, int64_t n) {
 lcvq_status_t lcvq_linear_fwd_int4(int64_t N, int64_t m, int64_t n, int32_t group, const uint8_t *packed,
                                    const void *scales, const void *zeros, const void *X, void *Y, int32_t y_dtype,
                                    void *workspace, size_t workspace_bytes, void *stream) {
+  return lcvq_linear_fwd_int4_ex(N, m, n, group, packed, scales, zeros, LCVQ_SCALES_BY_GROUP, X, Y, y_dtype, workspace,
+                                 workspace_bytes, stream);
+}
+
+lcvq_status_t lcvq_linear_fwd_int4_ex(int64_t N, int64_t m, int64_t n, int32_t group, const uint8_t *packed,
+                                      const void *scales, const void *zeros, int32_t scales_order, const void *X, void *Y,
+                                      int32_t y_dtype, void *workspace, size_t workspace_bytes, void *stream) {
   if (N < 0 || m < 0 || n < 0) return fail(LCVQ_EINVAL, "negative size (N=%lld m=%lld n=%lld)", (long long)N, (long long)m, (long long)n);
   if (N > kMaxTokens) return fail(LCVQ_EUNSUPPORTED, "N=%lld tokens (at most %lld per call)", (long long)N, (long long)kMaxTokens);
   if (group != 32 && group != 64 && (group <= 0 || group % 128 != 0))
@@ -1022,6 +1029,8 @@ lcvq_status_t lcvq_linear_fwd_int4(int64_t N, int64_t m, int64_t n, int32_t grou
   if (m >= kMaxLd || n >= kMaxLd) return fail(LCVQ_EUNSUPPORTED, "m or n above %lld", (long long)kMaxLd);
   if (n / group * m >= ((int64_t)1 << 30)) return fail(LCVQ_EUNSUPPORTED, "%lld groups (below 2^30)", (long long)(n / group * m));
   if (y_dtype != LCVQ_F32 && y_dtype != LCVQ_BF16) return fail(LCVQ_EINVAL, "y_dtype=%d", y_dtype);
+  if (scales_order != LCVQ_SCALES_BY_GROUP && scales_order != LCVQ_SCALES_BY_ROW)
+    return fail(LCVQ_EINVAL, "scales_order=%d", scales_order);
   if (N == 0 || m == 0) return ok();
   const size_t ys = y_dtype == LCVQ_BF16 ? 2 : 4;
   hipStream_t st = (hipStream_t)stream;
@@ -1036,7 +1045,8 @@ lcvq_status_t lcvq_linear_fwd_int4(int64_t N, int64_t m, int64_t n, int32_t grou
   const size_t need = lcvq_int4_workspace_bytes(N, m, n);
   if (need > 0 && (workspace == nullptr || workspace_bytes < need))
     return fail(LCVQ_EWORKSPACE, "workspace %zu bytes, need %zu", workspace_bytes, need);
-  lcvq::Int4Args a{packed, (const uint16_t *)scales, (const uint16_t *)zeros, m, n, group, y_dtype == LCVQ_BF16, (float *)workspace};
+  lcvq::Int4Args a{packed, (const uint16_t *)scales, (const uint16_t *)zeros, m, n, group, scales_order == LCVQ_SCALES_BY_ROW,
+                   y_dtype == LCVQ_BF16, (float *)workspace};
   for (int64_t t0 = 0; t0 < N; t0 += 16) {
     Timed tm(LCVQ_K_INT4, st);
     e = tm.done(lcvq::launch_int4(a, (const uint16_t *)X + t0 * n, (int)std::min<int64_t>(16, N - t0), (char *)Y + t0 * m * ys, st));

@@ -18,6 +18,12 @@
 // blocks as well (k_int4_sum adds those).  Each wave has two stages: the loads of the next
 // step are in flight while the current one is multiplied.
 //
+// Scales and zero points come in either order (strides): by row, as quantisers make them, a
+// step takes 2 kU bytes of a line of each row, which costs the first-level cache more lookups than
+// the codes do; by group its rows lie side by side.  By row / by group, a graph of calls:
+// 28672 x 8192 with zero points at one token 34.3 / 30.4 us, in groups of 32 41.0 / 37.8; 8192 x
+// 28672 in groups of 64 at 16 tokens 39.8 / 36.4; up to 11008 columns and rows no difference.
+//
 // Bound: HBM, the codes once (0.5 byte per weight, and 2 or 4 bytes per group); at 16 tokens
 // also X from the L2, as many bytes as the codes of 64 rows.  28672 x 8192 with zero points, one
 // token: 28 us, 4.5 TB/s; 8192 x 28672 in groups of 64, 16 tokens: 32 us, 3.9 TB/s, and 4 for the
@@ -58,16 +64,17 @@ __device__ __forceinline__ int int4_word(int i, int q) {
   return kG == 128 ? 4 * q + i : kG == 64 ? 8 * (i >> 1) + 2 * q + (i & 1) : 4 * i + q;
 }
 
-// kTok: tokens staged, 4 or 16.  kG: columns that a product's sum may span (32, 64, 128; larger groups are multiples of
+// Scale (and zero point) of row r and group k: element r s_row + k s_group.  kTok: tokens staged, 4 or 16.  kG: columns that a product's sum may span (32, 64, 128; larger groups are multiples of
 // 128).  kSplit: block (x, y) takes the steps [y span, (y + 1) span) and stores its sums in
 // `part` (span y, token, row).
 template <int MR, int kW, int kTok, int kG, bool kZero, bool kSplit>
 __global__ __launch_bounds__(64 * kW, MR > 4 ? 1 : 2) void k_int4(const uint8_t *__restrict__ packed, const uint16_t *__restrict__ scales,
-                                                     const uint16_t *__restrict__ zeros, int64_t m, int64_t n, int64_t groups, uint64_t per_step, int KT,
+                                                     const uint16_t *__restrict__ zeros, int64_t m, int64_t n, int64_t groups, uint32_t s_row,
+                                                     uint32_t s_group, uint64_t per_step, int KT,
                                                      const uint16_t *__restrict__ X, int Nc, void *__restrict__ Y, int y_bf16,
                                                      int span, float *__restrict__ part) {
   constexpr int kU = 128 / kG;                                   // groups of a step
-  constexpr int kS = (MR + 3) / 4, kP = kU * (kZero ? 2 : 1);    // loads of 64 rows' scales; such vectors of a step
+  constexpr int kS = (MR * kU + 3) / 4, kP = kZero ? 2 : 1;      // loads of a step's scales, and of its zero points
   constexpr int kX = MR * 1024 + kP * kS * 256, kStage = kX + kTok * 256;  // X behind codes and scales
   constexpr int kLoads = kTok / 4 + kP * kS + MR;
   __shared__ __attribute__((aligned(1024))) char lds[2 * kW * kStage];
@@ -82,8 +89,11 @@ __global__ __launch_bounds__(64 * kW, MR > 4 ? 1 : 2) void k_int4(const uint8_t 
   const __amdgpu_buffer_rsrc_t rsX = make_rsrc(X, (int64_t)Nc * n * 2);
   const int lrow = lane >> 2, lpiece = (lane & 3) ^ ((lrow >> 1) & 3);
   const uint32_t aoff = (uint32_t)(lrow * ldb + 16 * lpiece), astep = (uint32_t)(16 * ldb);
-  const __amdgpu_buffer_rsrc_t rsS = make_rsrc(scales + r0, (groups * m - r0) * 2);
-  const __amdgpu_buffer_rsrc_t rsZ = make_rsrc(kZero ? zeros + r0 : scales, kZero ? (groups * m - r0) * 2 : 0);
+  const int64_t s0 = r0 * s_row, s_bytes = (groups * m - s0) * 2;
+  const __amdgpu_buffer_rsrc_t rsS = make_rsrc(scales + s0, s_bytes);
+  const __amdgpu_buffer_rsrc_t rsZ = make_rsrc(kZero ? zeros + s0 : scales, kZero ? s_bytes : 0);
+
+  const uint32_t soff = 2u * ((uint32_t)(lane % kU) * s_group + (uint32_t)(lane / kU) * s_row);
 
   // A step past the end loads zeros; no load is behind a branch, so that their number is known.
   auto load = [&](int u, int j) __attribute__((always_inline)) {
@@ -99,20 +109,18 @@ __global__ __launch_bounds__(64 * kW, MR > 4 ? 1 : 2) void k_int4(const uint8_t 
       buffer_to_lds16(rsX, (lds_void *)(lds + base + kX + i * 1024),
                       on & (t < Nc) & (c < (int)n) ? (uint32_t)(t * (int)n + c) * 2u : kOffNone);
     }
-    // scales of the block's rows, one to a dword of LDS (rows past m: the next group's, not stored)
+    // The block's scales, one to a dword of LDS, a row's groups side by side: lanes of one row read
+    // one line where the scales are in rows, lanes of one group where they are in groups.  (Of
+    // rows past m what lies there, or zeros: not stored.  A group of 128 / kU columns, or of
+    // several steps: j / (group / 128) as a product.)
+    const uint32_t g0 = kU > 1 ? (uint32_t)(j * kU) : (uint32_t)(((uint64_t)(uint32_t)j * per_step) >> 32);
+    const uint32_t at = on & (j * 128 + (lane % kU) * kG < (int)n) ? 2u * (g0 * s_group) + soff : kOffNone;
 #pragma unroll
-    for (int k = 0; k < kU; ++k) {
-      // (a group of 128 / kU columns, or of several steps: j / (group / 128) as a product)
-      const uint32_t gi = kU > 1 ? (uint32_t)(j * kU + k) : (uint32_t)(((uint64_t)(uint32_t)j * per_step) >> 32);
-      const uint32_t off = on & (j * 128 + k * kG < (int)n) ? gi * (uint32_t)m * 2u + 2u * lane : kOffNone;
-#pragma unroll
-      for (int i = 0; i < kS; ++i) {
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(rsS, (lds_void *)(lds + base + MR * 1024 + (k * kS + i) * 256), 2,
-                                                 (int)(off + 128u * i), 0, 0, 0);
-        if constexpr (kZero)
-          __builtin_amdgcn_raw_ptr_buffer_load_lds(rsZ, (lds_void *)(lds + base + MR * 1024 + ((kU + k) * kS + i) * 256), 2,
-                                                   (int)(off + 128u * i), 0, 0, 0);
-      }
+    for (int i = 0; i < kS; ++i) {
+      const uint32_t off = lane < 16 * MR * kU - 64 * i ? at + (uint32_t)(128 / kU * i) * s_row : kOffNone;
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rsS, (lds_void *)(lds + base + MR * 1024 + i * 256), 2, (int)off, 0, 0, 0);
+      if constexpr (kZero)
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rsZ, (lds_void *)(lds + base + MR * 1024 + (kS + i) * 256), 2, (int)off, 0, 0, 0);
     }
     // a row's words past its end are its neighbour's, or zeros: they meet zeros of X
 #pragma unroll
@@ -160,19 +168,22 @@ __global__ __launch_bounds__(64 * kW, MR > 4 ? 1 : 2) void k_int4(const uint8_t 
           w[i] = *reinterpret_cast<const uint32_t *>(st + rb * 1024 + (((wd >> 2) ^ swz) << 4) + 4 * (wd & 3));
         }
       }
+      const u32x4 *vec = reinterpret_cast<const u32x4 *>(lds + base + MR * 1024 + (16 * rb + 4 * q) * kU * 4);
+      u32x4 sv[kU], zv[kU];  // of the lane's four rows and their groups: row e, group k in dword e kU + k
+#pragma unroll
+      for (int k = 0; k < kU; ++k) {
+        sv[k] = vec[k];
+        zv[k] = kZero ? vec[k + kS * 16] : u32x4{0u, 0u, 0u, 0u};
+      }
 #pragma unroll
       for (int k = 0; k < kU; ++k) {
         floatx4 acc = none;
 #pragma unroll
         for (int i = k * (4 / kU); i < (k + 1) * (4 / kU); ++i)
           acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(int4_operand(w[i]), xf[i], acc, 0, 0, 0);
-        const char *vec = lds + base + MR * 1024 + k * kS * 256 + (16 * rb + 4 * q) * 4;
-        const u32x4 s = *reinterpret_cast<const u32x4 *>(vec);
-        u32x4 z = {0u, 0u, 0u, 0u};
-        if constexpr (kZero) z = *reinterpret_cast<const u32x4 *>(vec + kU * kS * 256);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const uint32_t se = s[e], ze = z[e];
+          const uint32_t se = sv[(e * kU + k) / 4][(e * kU + k) % 4], ze = zv[(e * kU + k) / 4][(e * kU + k) % 4];
           const float t = kZero ? fmaf(-16.0f - bf16_to_f32((uint16_t)ze), off[k], acc[e]) : acc[e] - off[k];
           y[rb][e] = fmaf(bf16_to_f32((uint16_t)se), t, y[rb][e]);
         }
@@ -294,6 +305,7 @@ static hipError_t launch(const Int4Args &a, const uint16_t *X, int Nc, char *Y, 
   constexpr bool kMany = kTok == 16;
   constexpr int kMost = kMany ? 8 : 3;
   const Int4Plan p = int4_plan(a.m, a.n, kMany, kMost);
+  const int64_t groups = a.n / a.group;
   // ceil(2^32 / (group / 128)): exact for fewer than 2^14 steps
   const uint64_t per_step = ((1ull << 32) + std::max(a.group / 128, 1) - 1) / std::max(a.group / 128, 1);
   using K = decltype(&k_int4<1, 8, kTok, kG, kZero, false>);
@@ -316,7 +328,7 @@ static hipError_t launch(const Int4Args &a, const uint16_t *X, int Nc, char *Y, 
     f = k[p.mr - 1];
   }
   f<<<dim3((unsigned)ceil_div(a.m, 16 * p.mr), (unsigned)p.spans), 64 * waves, 0, st>>>(
-      a.packed, a.scales, a.zeros, a.m, a.n, a.n / a.group, per_step, p.KT, X, Nc, Y, a.y_bf16 ? 1 : 0, p.span, a.part);
+      a.packed, a.scales, a.zeros, a.m, a.n, groups, (uint32_t)(a.by_row ? groups : 1), (uint32_t)(a.by_row ? 1 : a.m), per_step, p.KT, X, Nc, Y, a.y_bf16 ? 1 : 0, p.span, a.part);
   if (p.spans > 1)
     k_int4_sum<<<(unsigned)ceil_div(a.m * Nc, 256), 256, 0, st>>>(a.part, p.spans, a.m * Nc, Y, a.y_bf16 ? 1 : 0);
   return hipGetLastError();

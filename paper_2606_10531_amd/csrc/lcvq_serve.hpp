@@ -88,6 +88,7 @@ struct Int4Args {
   const uint16_t *scales, *zeros;  // zeros: or nullptr
   int64_t m, n;
   int group;
+  bool by_row;  // scales and zeros: m x n / group, else n / group x m
   bool y_bf16;
   float *part;  // int4_bytes of the tokens of a pass
 };
