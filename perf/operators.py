@@ -201,9 +201,6 @@ def prepare(case, seed):
         c = c.reshape(m, n)
         s["packed"] = c[:, 0::2] | (c[:, 1::2] << 4)          # two codes a byte, the even column low
         s["scales"].mul_(1.0 / math.sqrt(n))                 # outputs near 1
-        s["scales"] = s["scales"].t().contiguous()           # a row of m per group
-        if case["zeros"]:
-            s["zeros"] = s["zeros"].t().contiguous()
         s["X"] = _normal(g, N, n).to(_BF16)
         s["out"] = torch.empty((N, m), dtype=torch.float32 if case["f32"] else _BF16, device="cuda")
         if own:
@@ -297,8 +294,7 @@ def _plain_attn(s):
 def _plain_int4(s):
     c = s["case"]
     w = torch.stack([s["packed"] & 15, s["packed"] >> 4], dim=-1).reshape(c["m"], -1, c["group"]).float()
-    w.sub_(8.0 if s["zeros"] is None else s["zeros"].float().t().unsqueeze(-1))
-    w.mul_(s["scales"].float().t().unsqueeze(-1))
+    w.sub_(8.0 if s["zeros"] is None else s["zeros"].float().unsqueeze(-1)).mul_(s["scales"].float().unsqueeze(-1))
     return torch.matmul(s["X"].float(), w.reshape(c["m"], c["n"]).t()).to(s["out"].dtype)
 
 
@@ -368,8 +364,8 @@ def exact(case, seed):
         zero = None if s["zeros"] is None else s["zeros"].cpu().double()
         for k in range(case["n"] // case["group"]):
             cols = slice(k * case["group"], (k + 1) * case["group"])
-            z = 8.0 if zero is None else zero[k][:, None]
-            y += (X[:, cols] @ (code[:, cols] - z).T) * scale[k]
+            z = 8.0 if zero is None else zero[:, k:k + 1]
+            y += (X[:, cols] @ (code[:, cols] - z).T) * scale[:, k]
         return y
     held = _decoded(s)
     if kind == "kv_read":
