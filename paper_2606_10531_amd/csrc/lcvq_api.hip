@@ -957,6 +957,9 @@ lcvq_status_t lcvq_attn_paged(int64_t T, int32_t B, int32_t Hq, int32_t Hkv, int
     return fail(LCVQ_EWORKSPACE, "workspace %zu bytes, need %zu", workspace_bytes, need);
   hipStream_t st = (hipStream_t)stream;
   max_q = (int32_t)std::min<int64_t>(max_q, T);
+  // a window that the table's tokens do not reach hides none (and stays below 2^30, so that the
+  // kernels' differences with lengths and rows fit 32 bits)
+  if (window >= table_width * page_size) window = 0;
   lcvq::AttnArgs a{};
   a.q = (const uint16_t *)q;
   a.q_token = q_token;
