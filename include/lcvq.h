@@ -455,8 +455,8 @@ lcvq_status_t lcvq_kv_read(int64_t T, int32_t Hkv, int32_t D, const int64_t *slo
  *   out       T x Hq x D bf16 dense;  lse  T x Hq fp32, or NULL
  *   max_q     no sequence has more new tokens than that; rows past it are not written
  * Array contents are bounded on the device: q_starts to [0, T], kv_lens to the table's
- * width.  Rows that belong to no sequence are not written.  Scores, statistics and sums
- * are fp32; probabilities are rounded to bf16 for the second product.
+ * width.  Rows that belong to no sequence are not written.  Scores q.k, their differences,
+ * statistics and sums are fp32; probabilities are rounded to bf16 for the second product.
  * Hq a multiple of Hkv, at most 64 heads on one; T * Hq below 2^30, B * Hkv below 2^23, table_width *
  * page_size below 2^30, scale positive, at most 1e6.  The workspace (16-byte aligned) is
  * lcvq_attn_workspace_bytes(..): one of that size serves every call of the same Hq, Hkv

@@ -8,8 +8,12 @@
 namespace lcvq {
 
 // Running maximum of a row that has seen nothing: finite, so that the factor of a hidden
-// score (-inf) is exp2(-inf) = 0 and never inf - inf.
-constexpr float kAttnLow = -1e30f;
+// score (-inf) is exp2(-inf) = 0 and never inf - inf, and no score lies below it.
+constexpr float kAttnLow = -3.402823466e38f;
+// A probability is exp2(c (x - m)), as one fma exp2(c x - [c m]).  The rounding of [c m] is then a
+// factor of all of a row's probabilities under one maximum, up to 2^(|c m| 2^-24): beyond
+// this |c m| the difference x - m is taken first, which is exact at the maximum and near it.
+constexpr float kAttnFar = 4096.0f;
 
 template <int N>
 __device__ __forceinline__ void attn_wait_vm() {
@@ -175,7 +179,7 @@ __device__ __forceinline__ float attn_sum4(float x) {
 }
 
 // Four elements d .. d + 3 of row r (new token r / G, query head h G + r % G): v / sum, and
-// with d == 0 the row's lse = ln(sum) + maximum (mx in log2 units).  A row that saw nothing
+// with d == 0 the row's lse = ln(sum) + scale times the maximum mx.  A row that saw nothing
 // gives 0 and -inf.
 __device__ __forceinline__ void attn_store(const AttnArgs &a, const AttnSeq &s, int h, int r, int d, int D, const floatx4 &v,
                                            float mx, float sum) {
@@ -185,7 +189,7 @@ __device__ __forceinline__ void attn_store(const AttnArgs &a, const AttnSeq &s, 
   const u32x2 w = {pack_bf16x2(v[0] * inv, v[1] * inv), pack_bf16x2(v[2] * inv, v[3] * inv)};
   *reinterpret_cast<u32x2 *>(a.out + row * D + d) = w;
   if (d == 0 && a.lse != nullptr)
-    a.lse[row] = sum == 0.0f ? -__builtin_inff() : (mx + __builtin_amdgcn_logf(sum)) * 0.69314718055994530942f;
+    a.lse[row] = sum == 0.0f ? -__builtin_inff() : fmaf(mx, a.c, __builtin_amdgcn_logf(sum)) * 0.69314718055994530942f;
 }
 
 // ---- values that are no numbers ------------------------------------------------

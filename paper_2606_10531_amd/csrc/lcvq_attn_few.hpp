@@ -25,7 +25,7 @@ __device__ __forceinline__ int64_t attn_share(int64_t total, int blocks, int p) 
   return p >= n ? total : total * p / n;
 }
 
-// One partial result: 16 NB rows of D sums, then their maxima (log2 units), then their sums.
+// One partial result: 16 NB rows of D sums, then their maxima, then their sums.
 template <int D, int NB>
 __device__ __forceinline__ constexpr int64_t part_floats() {
   return (int64_t)16 * NB * (D + 2);
@@ -234,7 +234,12 @@ __device__ __forceinline__ void attn_few(const AttnArgs &a, char *lds, int p, in
 #pragma unroll
           for (int db = 0; db < D / 16; ++db) acc[db][n] *= f;
         }
-        const float mc = m[n] * a.c;
+        float mc = m[n] * a.c;
+        if (__ballot(fabsf(mc) > kAttnFar)) {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) x[j] -= m[n];
+          mc = 0.0f;
+        }
         float pr[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
@@ -297,7 +302,6 @@ __device__ __forceinline__ void attn_few(const AttnArgs &a, char *lds, int p, in
 #pragma unroll
     for (int n = 0; n < NB; ++n) {
       l[n] = attn_sum4(l[n]);
-      m[n] *= a.c;  // log2 units
       if (g == 0) {
         s_m[wave][16 * n + c16] = m[n];
         s_l[wave][16 * n + c16] = l[n];
@@ -309,7 +313,7 @@ __device__ __forceinline__ void attn_few(const AttnArgs &a, char *lds, int p, in
 #pragma unroll
     for (int n = 0; n < NB; ++n) {
       const int r = 16 * n + c16;
-      f[n] = __builtin_amdgcn_exp2f(m[n] - fmaxf(fmaxf(s_m[0][r], s_m[1][r]), fmaxf(s_m[2][r], s_m[3][r])));
+      f[n] = __builtin_amdgcn_exp2f((m[n] - fmaxf(fmaxf(s_m[0][r], s_m[1][r]), fmaxf(s_m[2][r], s_m[3][r]))) * a.c);
     }
     const bool whole = kWhole || (pos == unit0 && stop == unit0 + nb_);
     if (!kWhole && tid == 0) {  // where the unit's pieces are, for k_attn_join
@@ -336,7 +340,7 @@ __device__ __forceinline__ void attn_few(const AttnArgs &a, char *lds, int p, in
         const float mx = fmaxf(fmaxf(s_m[0][r], s_m[1][r]), fmaxf(s_m[2][r], s_m[3][r]));
         float sum = 0.0f;
 #pragma unroll
-        for (int w = 0; w < 4; ++w) sum += s_l[w][r] * __builtin_amdgcn_exp2f(s_m[w][r] - mx);
+        for (int w = 0; w < 4; ++w) sum += s_l[w][r] * __builtin_amdgcn_exp2f((s_m[w][r] - mx) * a.c);
         const int d = half * kDh + d0;
         if (whole) {
           attn_store(a, sq, h, r, d, D, v, mx, sum);
@@ -364,7 +368,7 @@ __device__ __forceinline__ void attn_few(const AttnArgs &a, char *lds, int p, in
   }
 }
 
-// ---- joining the pieces of a unit: their sums, maxima (log2 units) and sums of exponentials.
+// ---- joining the pieces of a unit: their sums, maxima and sums of exponentials.
 // kShare groups of threads take the same rows of different pieces and add up in LDS, so that
 // 27 pieces (the most of a chunk's) are 7 rounds of loads.
 template <int D, int kShare>
@@ -389,7 +393,7 @@ __device__ __forceinline__ void attn_join(const AttnArgs &a, char *lds, const At
     const float *part = piece(i);
     const floatx4 x = *reinterpret_cast<const floatx4 *>(part + (int64_t)r * D + d0);
     const float pm = part[kPiece * D + r], psum = part[kPiece * D + kPiece + r];
-    const float mn = fmaxf(m, pm), f = __builtin_amdgcn_exp2f(m - mn), fp = __builtin_amdgcn_exp2f(pm - mn);
+    const float mn = fmaxf(m, pm), f = __builtin_amdgcn_exp2f((m - mn) * a.c), fp = __builtin_amdgcn_exp2f((pm - mn) * a.c);
     v = v * f + x * fp;
     l = l * f + psum * fp;
     m = mn;
@@ -412,7 +416,7 @@ __device__ __forceinline__ void attn_join(const AttnArgs &a, char *lds, const At
     v = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
     for (int i = 0; i < kShare; ++i) {
-      const float f = __builtin_amdgcn_exp2f(s_m[i][rl] - m);
+      const float f = __builtin_amdgcn_exp2f((s_m[i][rl] - m) * a.c);
       v += red[i][rl][tid % kT] * f;
       l += s_l[i][rl] * f;
     }

@@ -22,7 +22,8 @@
 // unit (168 registers) are no faster than two.
 //
 // The running maximum follows only when a row's has grown by 8 in log2 units, so that
-// probabilities reach at most 2^8 and the rescaling branch is rare.
+// probabilities reach at most 2^8 and the rescaling branch is rare.  (Under the true maximum the
+// largest probability is 1, which bf16 holds; under a lagging one it is rounded like the others.)
 //
 // Blocks of one cached head follow one another every Hkv blocks, so that with 8 (16, ..)
 // heads an XCD's L2 holds its own head's entries; long units come first.
@@ -116,11 +117,12 @@ __device__ __forceinline__ void attn_wide(const AttnArgs &a, char *lds, int bloc
   const int tiles = tb - ta, tok0 = (tile0 + ta) * kWideTok;
 
   floatx4 acc[D / 16][NB];
+  bool far = true;  // some row's |c m| is beyond kAttnFar: its exponents are c (x - m), and mc is 0
   float m[NB], mc[NB], l[NB];
 #pragma unroll
   for (int n = 0; n < NB; ++n) {
     m[n] = kAttnLow;
-    mc[n] = kAttnLow * a.c;
+    mc[n] = 0.0f;
     l[n] = 0.0f;
 #pragma unroll
     for (int db = 0; db < D / 16; ++db) acc[db][n] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
@@ -206,20 +208,27 @@ __device__ __forceinline__ void attn_wide(const AttnArgs &a, char *lds, int bloc
   // mx: maxima of a tile's scores over the lane's tokens.  New running maxima where a row's has
   // grown by more than the slack.
   auto follow = [&](float (&mx)[NB]) __attribute__((always_inline)) {
-    float over = fmaf(mx[0], a.c, -mc[0]);
+    float over = (mx[0] - m[0]) * a.c;
 #pragma unroll
-    for (int n = 1; n < NB; ++n) over = fmaxf(over, fmaf(mx[n], a.c, -mc[n]));
+    for (int n = 1; n < NB; ++n) over = fmaxf(over, (mx[n] - m[n]) * a.c);
     if (__ballot(over > kWideSlack) == 0) return;
+    float most = 0.0f;
 #pragma unroll
     for (int n = 0; n < NB; ++n) {
       const float mn = fmaxf(m[n], attn_max4(mx[n])), f = __builtin_amdgcn_exp2f((m[n] - mn) * a.c);
       m[n] = mn;
       mc[n] = mn * a.c;
+      most = fmaxf(most, fabsf(mc[n]));
       l[n] *= f;
 #pragma unroll
       for (int db = 0; db < D / 16; ++db) acc[db][n] *= f;
     }
-    };
+    far = __ballot(most > kAttnFar) != 0;
+    if (far) {
+#pragma unroll
+      for (int n = 0; n < NB; ++n) mc[n] = 0.0f;
+    }
+  };
 
   constexpr int kKs = D / 32, kDb = D / 16;
   // Tile i on the pages id0.  K(i + 1) and V(i + 1) are under way; those of i + 2, on id2, take
@@ -246,6 +255,14 @@ __device__ __forceinline__ void attn_wide(const AttnArgs &a, char *lds, int bloc
       for (int j = 1; j < 16; ++j) mx[n] = wide_max(mx[n], s[j >> 2][n][j & 3]);
     }
     follow(mx);
+    if (far) {
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+#pragma unroll
+        for (int n = 0; n < NB; ++n)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s[u][n][e] -= m[n];
+    }
     bf16x8 pf[2][NB];
 #pragma unroll
     for (int k = 0; k < 2; ++k)
@@ -314,13 +331,13 @@ __device__ __forceinline__ void attn_wide(const AttnArgs &a, char *lds, int bloc
     if (r >= rows) continue;
     if (splits == 1) {
 #pragma unroll
-      for (int db = 0; db < D / 16; ++db) attn_store(a, sq, h, r, 16 * db + 4 * g, D, acc[db][n], mc[n], l[n]);
+      for (int db = 0; db < D / 16; ++db) attn_store(a, sq, h, r, 16 * db + 4 * g, D, acc[db][n], m[n], l[n]);
     } else {
       float *part = a.part_wide + (((int64_t)item * a.Hkv + h) * splits + split) * wide_part_floats<D>();
 #pragma unroll
       for (int db = 0; db < D / 16; ++db) *reinterpret_cast<floatx4 *>(part + (int64_t)(r - r0) * D + 16 * db + 4 * g) = acc[db][n];
       if (g == 0) {
-        part[kAttnWideRows * D + r - r0] = mc[n];
+        part[kAttnWideRows * D + r - r0] = m[n];
         part[kAttnWideRows * D + kAttnWideRows + r - r0] = l[n];
       }
     }

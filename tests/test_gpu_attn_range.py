@@ -1,7 +1,10 @@
 """Attention over the paged cache at the ends of its arguments' ranges.  The tolerances are those of
 the attention tests."""
+import numpy as np
 import pytest
 import test_gpu_attn as attn
+
+from oracle import serve
 
 pytestmark = pytest.mark.gpu
 
@@ -21,3 +24,47 @@ def test_windows_longer_than_any_table(lc, seqs, fp8, window):
     c.check(out, lse)
     want = c.call(lc)
     assert out.equal(want[0]) and lse.equal(want[1])
+
+
+def _whole_numbers(seqs, fp8, q0, k0, qi, ki, seed):
+    """A case whose scores are exact in 32 bits: q and k are q0 and k0 in the first element and whole
+    numbers from -3 to 3 times qi and ki in the others."""
+    import torch
+    c = attn.Case(seqs, 4, 2, 64, 16, fp8, seed=seed)
+    rng = np.random.default_rng(seed)
+    k = rng.integers(-3, 4, c.kv[0].shape) * float(ki)
+    k[..., 0] = k0
+    if fp8:
+        codes, scales = serve.kv_encode(k)
+        assert np.array_equal(serve.kv_decode(codes, scales), k)
+        c.data[0], c.scales[0] = torch.from_numpy(codes).cuda(), torch.from_numpy(scales).cuda()
+    else:
+        c.data[0] = torch.from_numpy(k).to(torch.bfloat16).cuda()
+    c.kv[0] = k
+    q = rng.integers(-3, 4, c.q.shape) * float(qi)
+    q[..., 0] = q0
+    c.q = torch.from_numpy(q).to(torch.bfloat16).cuda()
+    return c
+
+
+SEQS = [[(1, 300), (2, 45)], [(90, 200), (1, 130)], [(1, 3000)], [(40, 1500)]]
+
+
+@pytest.mark.parametrize("fp8", [True, False])
+@pytest.mark.parametrize("seqs", SEQS)
+@pytest.mark.parametrize("e", [105, 127])
+def test_scores_far_below_zero(lc, seqs, e, fp8):
+    """q.k about -2^105 or -2^127 in every row, scaled to -256 and some tens around it."""
+    c = _whole_numbers(seqs, fp8, 2.0 ** (e // 2 + 1), -2.0 ** (e - e // 2 - 1), 2.0 ** (e // 2 - 5), 2.0 ** (e - e // 2 - 5), 31)
+    out, lse = c.call(lc, scale=2.0 ** (8 - e))
+    c.check(out, lse, scale=2.0 ** (8 - e))
+
+
+@pytest.mark.parametrize("fp8", [True, False])
+@pytest.mark.parametrize("seqs", SEQS)
+@pytest.mark.parametrize("common,scale", [(1024, 1.0), (1024, 0.03), (1024, 1e6), (64, 1e6), (0, 7e5), (0, 1e-30)])
+def test_large_scaled_scores(lc, seqs, common, scale, fp8):
+    """Scores of up to 10^12: what counts is by how much they differ."""
+    c = _whole_numbers(seqs, fp8, common, common, 1, 1, 32)
+    out, lse = c.call(lc, scale=scale)
+    c.check(out, lse, scale=scale)
