@@ -235,10 +235,12 @@ __device__ __forceinline__ void attn_few(const AttnArgs &a, char *lds, int p, in
           for (int db = 0; db < D / 16; ++db) acc[db][n] *= f;
         }
         float mc = m[n] * a.c;
-        if (__ballot(fabsf(mc) > kAttnFar)) {
+        const bool far = fabsf(mc) > kAttnFar;
+        if (__ballot(far)) {  // (other rows keep their bits)
+          const float off = far ? m[n] : 0.0f;
 #pragma unroll
-          for (int j = 0; j < 8; ++j) x[j] -= m[n];
-          mc = 0.0f;
+          for (int j = 0; j < 8; ++j) x[j] -= off;
+          mc = far ? 0.0f : mc;
         }
         float pr[8];
 #pragma unroll

@@ -117,12 +117,14 @@ __device__ __forceinline__ void attn_wide(const AttnArgs &a, char *lds, int bloc
   const int tiles = tb - ta, tok0 = (tile0 + ta) * kWideTok;
 
   floatx4 acc[D / 16][NB];
-  bool far = true;  // some row's |c m| is beyond kAttnFar: its exponents are c (x - m), and mc is 0
+  // mc: c m, or 0 where |c m| is beyond kAttnFar and the exponents are c (x - m); far: some row's is
+  auto near_mc = [&](float x) __attribute__((always_inline)) { return fabsf(x * a.c) > kAttnFar ? 0.0f : x * a.c; };
+  bool far = true;
   float m[NB], mc[NB], l[NB];
 #pragma unroll
   for (int n = 0; n < NB; ++n) {
     m[n] = kAttnLow;
-    mc[n] = 0.0f;
+    mc[n] = near_mc(kAttnLow);
     l[n] = 0.0f;
 #pragma unroll
     for (int db = 0; db < D / 16; ++db) acc[db][n] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
@@ -217,17 +219,13 @@ __device__ __forceinline__ void attn_wide(const AttnArgs &a, char *lds, int bloc
     for (int n = 0; n < NB; ++n) {
       const float mn = fmaxf(m[n], attn_max4(mx[n])), f = __builtin_amdgcn_exp2f((m[n] - mn) * a.c);
       m[n] = mn;
-      mc[n] = mn * a.c;
-      most = fmaxf(most, fabsf(mc[n]));
+      mc[n] = near_mc(mn);
+      most = fmaxf(most, fabsf(mn * a.c));
       l[n] *= f;
 #pragma unroll
       for (int db = 0; db < D / 16; ++db) acc[db][n] *= f;
     }
     far = __ballot(most > kAttnFar) != 0;
-    if (far) {
-#pragma unroll
-      for (int n = 0; n < NB; ++n) mc[n] = 0.0f;
-    }
   };
 
   constexpr int kKs = D / 32, kDb = D / 16;
@@ -257,11 +255,13 @@ __device__ __forceinline__ void attn_wide(const AttnArgs &a, char *lds, int bloc
     follow(mx);
     if (far) {
 #pragma unroll
-      for (int u = 0; u < 4; ++u)
+      for (int n = 0; n < NB; ++n) {
+        const float off = fabsf(m[n] * a.c) > kAttnFar ? m[n] : 0.0f;
 #pragma unroll
-        for (int n = 0; n < NB; ++n)
+        for (int u = 0; u < 4; ++u)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) s[u][n][e] -= m[n];
+          for (int e = 0; e < 4; ++e) s[u][n][e] -= off;
+      }
     }
     bf16x8 pf[2][NB];
 #pragma unroll

@@ -68,3 +68,16 @@ def test_large_scaled_scores(lc, seqs, common, scale, fp8):
     c = _whole_numbers(seqs, fp8, common, common, 1, 1, 32)
     out, lse = c.call(lc, scale=scale)
     c.check(out, lse, scale=scale)
+
+
+@pytest.mark.parametrize("fp8", [True, False])
+@pytest.mark.parametrize("seqs", [[(1, 300), (2, 45)], [(1, 3000)], [(3, 2000)]])
+def test_large_scores_of_one_row_leave_the_others_bits(lc, seqs, fp8):
+    """Few rows: one query a hundred thousand times larger than those beside it."""
+    c = attn.Case(seqs, 4, 2, 64, 16, fp8, seed=35)
+    want = c.call(lc)
+    c.q[0, 1] *= 1e5
+    out, lse = c.call(lc)
+    keep = [(t, h) for t in range(c.q.shape[0]) for h in range(4) if (t, h) != (0, 1)]
+    for t, h in keep:
+        assert out[t, h].equal(want[0][t, h]) and lse[t, h].equal(want[1][t, h]), (t, h)
