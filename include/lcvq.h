@@ -450,7 +450,8 @@ lcvq_status_t lcvq_kv_read(int64_t T, int32_t Hkv, int32_t D, const int64_t *slo
  *     out = sum_j softmax_j(scale q.k_j) v_j,   lse = ln sum_j exp(scale q.k_j)
  *   A row that sees nothing gets out 0 and lse -inf.  Tokens on a page outside
  *   [0, pages) (-1: not there) are hidden; nothing behind kv_lens is used, whatever
- *   the cache holds there.
+ *   the cache holds there, and what it holds for a hidden token (NaN, infinities, scale
+ *   bytes that the format has not) reaches no row that does not see it.
  *   q         bf16, element (t, h, i) at t * q_token + h * q_head + i (16-byte multiples)
  *   out       T x Hq x D bf16 dense;  lse  T x Hq fp32, or NULL
  *   max_q     no sequence has more new tokens than that; rows past it are not written

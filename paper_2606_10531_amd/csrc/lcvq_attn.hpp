@@ -196,7 +196,8 @@ __device__ __forceinline__ void attn_store(const AttnArgs &a, const AttnSeq &s, 
 // A token that some rows of a block see and others do not must not reach the others, but 0
 // times a NaN or an infinity is NaN.  Where a partly hidden tile of V holds such values they
 // are replaced by zeros before the product, and what they add is put in behind the
-// block's results (attn_put_odd).  Such a value in the entries' words, and the words without:
+// block's results (attn_put_odd).  An entry whose scale byte the format has not (its values may
+// reach infinity) counts as one of NaNs.  Such a value in the entries' words, and the words without:
 template <bool kFp8>
 __device__ __forceinline__ bool attn_odd(const u32x4 &w) {
   uint32_t odd = 0;
@@ -246,7 +247,7 @@ __device__ __forceinline__ void attn_put_odd(const AttnArgs &a, const AttnSeq &s
       const int64_t at = (((((int64_t)id * a.Hkv + h) << a.page_shift) + (t & ((1 << a.page_shift) - 1)))) * D + d;
       float v = 0.0f;
       if constexpr (kFp8) {
-        if ((reinterpret_cast<const uint8_t *>(a.v)[at] & 0x7fu) == 0x7fu) v = __builtin_nanf("");
+        if ((reinterpret_cast<const uint8_t *>(a.v)[at] & 0x7fu) == 0x7fu || a.vs[at / D] > kKvByteTop) v = __builtin_nanf("");
       } else {
         const uint16_t w = reinterpret_cast<const uint16_t *>(a.v)[at];
         if ((w & 0x7f80u) == 0x7f80u) v = bf16_to_f32(w);

@@ -181,11 +181,17 @@ __device__ __forceinline__ void attn_wide(const AttnArgs &a, char *lds, int bloc
     if ((t0 >= blk_lo) & (t0 + kWideTok <= blk_hi)) return;
     bool any = false;
 #pragma unroll
-    for (int j = 0; j < kC; ++j) any |= attn_odd<kFp8>(hold[1][j]);
+    for (int j = 0; j < kC; ++j) any |= attn_odd<kFp8>(hold[1][j]) || (kFp8 && hold_s[1][j] > kKvByteTop);
     if (__ballot(any) == 0) return;
     odd = true;
 #pragma unroll
-    for (int j = 0; j < kC; ++j) hold[1][j] = attn_without_odd<kFp8>(hold[1][j]);
+    for (int j = 0; j < kC; ++j) {
+      hold[1][j] = attn_without_odd<kFp8>(hold[1][j]);
+      if (kFp8 && hold_s[1][j] > kKvByteTop) {
+        hold[1][j] = u32x4{0u, 0u, 0u, 0u};
+        hold_s[1][j] = 127;
+      }
+    }
   };
   // ---- operands
   auto k_operand = [&](int buf, int u, int ks) __attribute__((always_inline)) {

@@ -14,6 +14,7 @@ namespace lcvq {
 // costs up to one bit of the codes' range against amax / 448, which e4m3's own exponents
 // take up, and makes both directions exact but for the one rounding of a code.
 constexpr int kKvExpLo = -117, kKvExpHi = 119;
+constexpr uint32_t kKvByteTop = 127 + kKvExpHi;  // the largest scale byte
 constexpr float kE4m3Max = 448.0f;
 
 // e from the bits of |amax| (finite): 448 = 1.75 2^8.

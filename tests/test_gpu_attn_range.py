@@ -81,3 +81,26 @@ def test_large_scores_of_one_row_leave_the_others_bits(lc, seqs, fp8):
     keep = [(t, h) for t in range(c.q.shape[0]) for h in range(4) if (t, h) != (0, 1)]
     for t, h in keep:
         assert out[t, h].equal(want[0][t, h]) and lse[t, h].equal(want[1][t, h]), (t, h)
+
+
+@pytest.mark.parametrize("byte", [247, 254, 255])
+@pytest.mark.parametrize("seqs", [[(4, 160), (1, 40)], [(90, 220), (1, 40)], [(90, 220)], [(150, 1500)]])
+@pytest.mark.parametrize("window,back", [(0, 2), (0, 45), (50, 45), (50, 51), (50, 100)])
+@pytest.mark.parametrize("keys", [False, True])
+def test_scale_bytes_that_the_format_has_not(lc, keys, seqs, window, back, byte):
+    """... of a token that some rows see (`back` before the last): the others are as without it,
+    to the bit where it is the value's and their scores and maxima are the same."""
+    c = attn.Case(seqs, 4, 2, 128, 16, True, seed=33)
+    n, length = seqs[0]
+    t = length - 1 - back
+    clean = c.call(lc, window=window)
+    c.scales[0 if keys else 1, c.table[0, t // 16], :, t % 16] = byte
+    out, lse = c.call(lc, window=window)
+    blind = [i for i in range(n) if not (t <= length - n + i and (window == 0 or t > length - n + i - window))]
+    rows = blind + list(range(n, c.q.shape[0]))
+    if not keys:
+        for i in rows:
+            assert out[i].equal(clean[0][i]) and lse[i].equal(clean[1][i]), i
+    out[[i for i in range(n) if i not in blind]] = clean[0][[i for i in range(n) if i not in blind]]
+    lse[[i for i in range(n) if i not in blind]] = clean[1][[i for i in range(n) if i not in blind]]
+    c.check(out, lse, window=window)
