@@ -14,6 +14,7 @@ constexpr float kAttnLow = -3.402823466e38f;
 // factor of all of a row's probabilities under one maximum, up to 2^(|c m| 2^-24): beyond
 // this |c m| the difference x - m is taken first, which is exact at the maximum and near it.
 constexpr float kAttnFar = 4096.0f;
+__device__ __forceinline__ bool attn_far(float m, float c) { return fabsf(m * c) > kAttnFar; }
 
 template <int N>
 __device__ __forceinline__ void attn_wait_vm() {

@@ -135,10 +135,12 @@ __device__ __forceinline__ void attn_few(const AttnArgs &a, char *lds, int p, in
     attn_range(a, sq, sq.nq - 1, all_lo, none);
 
     floatx4 acc[D / 16][NB];
-    float m[NB], l[NB];
+    float m[NB], mc[NB], l[NB];  // mc: c m, or 0 where that is far and the exponents are c (x - m)
+    uint32_t far = (1u << NB) - 1;  // the n some of whose rows are far
 #pragma unroll
     for (int n = 0; n < NB; ++n) {
       m[n] = kAttnLow;
+      mc[n] = attn_far(kAttnLow, a.c) ? 0.0f : kAttnLow * a.c;
       l[n] = 0.0f;
 #pragma unroll
       for (int db = 0; db < D / 16; ++db) acc[db][n] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
@@ -230,22 +232,21 @@ __device__ __forceinline__ void attn_few(const AttnArgs &a, char *lds, int p, in
         if (__ballot(mx > m[n])) {
           const float mn = fmaxf(m[n], mx), f = __builtin_amdgcn_exp2f((m[n] - mn) * a.c);
           m[n] = mn;
+          mc[n] = attn_far(mn, a.c) ? 0.0f : mn * a.c;
+          far = __ballot(attn_far(mn, a.c)) != 0 ? far | 1u << n : far & ~(1u << n);
           l[n] *= f;
 #pragma unroll
           for (int db = 0; db < D / 16; ++db) acc[db][n] *= f;
         }
-        float mc = m[n] * a.c;
-        const bool far = fabsf(mc) > kAttnFar;
-        if (__ballot(far)) {  // (other rows keep their bits)
-          const float off = far ? m[n] : 0.0f;
+        if (far >> n & 1) {  // (rows that are not keep their bits)
+          const float off = attn_far(m[n], a.c) ? m[n] : 0.0f;
 #pragma unroll
           for (int j = 0; j < 8; ++j) x[j] -= off;
-          mc = far ? 0.0f : mc;
         }
         float pr[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          pr[j] = __builtin_amdgcn_exp2f(fmaf(x[j], a.c, -mc));
+          pr[j] = __builtin_amdgcn_exp2f(fmaf(x[j], a.c, -mc[n]));
           l[n] += pr[j];
           if (kFp8) pr[j] *= vs8[j];
           if (masked) pr[j] = (seen >> j) & 1 ? pr[j] : 0.0f;

@@ -117,14 +117,13 @@ __device__ __forceinline__ void attn_wide(const AttnArgs &a, char *lds, int bloc
   const int tiles = tb - ta, tok0 = (tile0 + ta) * kWideTok;
 
   floatx4 acc[D / 16][NB];
-  // mc: c m, or 0 where |c m| is beyond kAttnFar and the exponents are c (x - m); far: some row's is
-  auto near_mc = [&](float x) __attribute__((always_inline)) { return fabsf(x * a.c) > kAttnFar ? 0.0f : x * a.c; };
+  // mc: c m, or 0 where that is far and the exponents are c (x - m); far: some row's is
   bool far = true;
   float m[NB], mc[NB], l[NB];
 #pragma unroll
   for (int n = 0; n < NB; ++n) {
     m[n] = kAttnLow;
-    mc[n] = near_mc(kAttnLow);
+    mc[n] = attn_far(kAttnLow, a.c) ? 0.0f : kAttnLow * a.c;
     l[n] = 0.0f;
 #pragma unroll
     for (int db = 0; db < D / 16; ++db) acc[db][n] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
@@ -220,18 +219,18 @@ __device__ __forceinline__ void attn_wide(const AttnArgs &a, char *lds, int bloc
 #pragma unroll
     for (int n = 1; n < NB; ++n) over = fmaxf(over, (mx[n] - m[n]) * a.c);
     if (__ballot(over > kWideSlack) == 0) return;
-    float most = 0.0f;
+    bool any_far = false;
 #pragma unroll
     for (int n = 0; n < NB; ++n) {
       const float mn = fmaxf(m[n], attn_max4(mx[n])), f = __builtin_amdgcn_exp2f((m[n] - mn) * a.c);
       m[n] = mn;
-      mc[n] = near_mc(mn);
-      most = fmaxf(most, fabsf(mn * a.c));
+      mc[n] = attn_far(mn, a.c) ? 0.0f : mn * a.c;
+      any_far |= attn_far(mn, a.c);
       l[n] *= f;
 #pragma unroll
       for (int db = 0; db < D / 16; ++db) acc[db][n] *= f;
     }
-    far = __ballot(most > kAttnFar) != 0;
+    far = __ballot(any_far) != 0;
   };
 
   constexpr int kKs = D / 32, kDb = D / 16;
@@ -262,7 +261,7 @@ __device__ __forceinline__ void attn_wide(const AttnArgs &a, char *lds, int bloc
     if (far) {
 #pragma unroll
       for (int n = 0; n < NB; ++n) {
-        const float off = fabsf(m[n] * a.c) > kAttnFar ? m[n] : 0.0f;
+        const float off = attn_far(m[n], a.c) ? m[n] : 0.0f;
 #pragma unroll
         for (int u = 0; u < 4; ++u)
 #pragma unroll
