@@ -227,36 +227,70 @@ __device__ __forceinline__ u32x4 attn_without_odd(const u32x4 &w) {
   }
   return r;
 }
-// For rows r0 .. r1 - 1 and the tokens from .. to - 1 that each sees: the sum of such values,
-// where there are any, through put(r, d, sum) (NaN or an infinity).  256 threads.
+// Element d of token t: 0 a number (or no such page), else one in the place of its kind's count: a
+// NaN, infinity, -infinity.  (Some page is there, or nothing had been left out.)
+constexpr int kAttnNan = 1, kAttnInf = 1 << 10, kAttnNegInf = 1 << 20;
+template <int D, bool kFp8>
+__device__ __forceinline__ int attn_odd_kind(const AttnArgs &a, int b, int h, int d, int t) {
+  const int id = a.table[(int64_t)b * a.width + (t >> a.page_shift)];
+  const bool there = (uint32_t)id < (uint32_t)a.pages;
+  const int64_t row = (((int64_t)(there ? id : 0) * a.Hkv + h) << a.page_shift) + (t & ((1 << a.page_shift) - 1));
+  if constexpr (kFp8) {
+    const uint32_t v = reinterpret_cast<const uint8_t *>(a.v)[row * D + d], scale = a.vs[row];
+    return there && ((v & 0x7fu) == 0x7fu || scale > kKvByteTop) ? kAttnNan : 0;
+  } else {
+    const uint32_t v = reinterpret_cast<const uint16_t *>(a.v)[row * D + d];
+    return !there || (v & 0x7f80u) != 0x7f80u ? 0 : (v & 0x7fu) != 0 ? kAttnNan : (v & 0x8000u) != 0 ? kAttnNegInf : kAttnInf;
+  }
+}
+// For rows r0 .. r1 - 1: the sum of such values among the tokens from .. to - 1 that each sees, where
+// there are any, through put(r, d, sum) (NaN or an infinity).  256 threads; a thread takes an
+// element of some rows in order, whose first and last tokens never fall: each token comes in
+// once and goes out once, four loads at a time.
 template <int D, bool kFp8, class Put>
-__device__ __forceinline__ void attn_put_odd(const AttnArgs &a, const AttnSeq &s, int b, int h, int r0, int r1, int from, int to,
-                                             Put put) {
+__device__ __forceinline__ void attn_put_odd_of(const AttnArgs &a, const AttnSeq &s, int b, int h, int r0, int r1, int from, int to,
+                                                Put put) {
+  constexpr int kParts = 256 / D;
+  const int d = threadIdx.x % D, per = (r1 - r0 + kParts - 1) / kParts;
+  const int ra = r0 + (int)threadIdx.x / D * per, rb = min(r1, ra + per);
+  int first = from, last = from, kinds = 0;  // the counts of the tokens first .. last - 1
+  auto move = [&](int &t, int end, int sign) __attribute__((always_inline)) {
 #pragma unroll 1
-  for (int it = threadIdx.x; it < (r1 - r0) * D; it += 256) {
-    const int r = r0 + it / D, d = it % D;
+    while (t < end) {
+      int k[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) k[j] = attn_odd_kind<D, kFp8>(a, b, h, d, min(t + j, end - 1));
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (t + j < end) kinds += sign * k[j];
+      t = min(t + 4, end);
+    }
+  };
+#pragma unroll 1
+  for (int r = ra; r < rb; ++r) {
     int lo, hi;
     attn_range(a, s, r / a.G, lo, hi);
-    lo = max(lo, from);
-    hi = min(hi, to);
-    float sum = 0.0f;
-    bool any = false;
+    lo = max(from, min(lo, to));
+    hi = max(lo, min(hi, to));
+    move(last, hi, 1);
+    move(first, lo, -1);
+    if (kinds == 0) continue;
+    const bool nan = (kinds & 1023) != 0, inf = (kinds >> 10 & 1023) != 0, neg = kinds >> 20 != 0;
+    put(r, d, nan || (inf && neg) ? __builtin_nanf("") : neg ? -__builtin_inff() : __builtin_inff());
+  }
+}
+// Of a block whose tiles of kTile tokens stand at from .. to - 1, and of whose tokens every row sees
+// all_lo .. all_hi - 1: values are left out of tiles before and behind these alone (at most a tile
+// and the rows' tokens each, or the window and the rows').
+template <int D, bool kFp8, int kTile, class Put>
+__device__ __forceinline__ void attn_put_odd(const AttnArgs &a, const AttnSeq &s, int b, int h, int r0, int r1, int from, int to,
+                                             int all_lo, int all_hi, Put put) {
+  int end = max(from, min(to, (all_lo + kTile - 1) & -kTile));
 #pragma unroll 1
-    for (int t = lo; t < hi; ++t) {
-      const int id = a.table[(int64_t)b * a.width + (t >> a.page_shift)];
-      if ((uint32_t)id >= (uint32_t)a.pages) continue;
-      const int64_t at = (((((int64_t)id * a.Hkv + h) << a.page_shift) + (t & ((1 << a.page_shift) - 1)))) * D + d;
-      float v = 0.0f;
-      if constexpr (kFp8) {
-        if ((reinterpret_cast<const uint8_t *>(a.v)[at] & 0x7fu) == 0x7fu || a.vs[at / D] > kKvByteTop) v = __builtin_nanf("");
-      } else {
-        const uint16_t w = reinterpret_cast<const uint16_t *>(a.v)[at];
-        if ((w & 0x7f80u) == 0x7f80u) v = bf16_to_f32(w);
-      }
-      any |= v != 0.0f;
-      sum += v;
-    }
-    if (any) put(r, d, sum);
+  for (int e = 0; e < 2; ++e) {
+    attn_put_odd_of<D, kFp8>(a, s, b, h, r0, r1, from, end, put);
+    from = min(to, max(end, all_hi & -kTile));
+    end = to;
   }
 }
 // ... into a finished row (whose element may be no number by itself: it stays one).

@@ -255,12 +255,12 @@ __device__ __forceinline__ void attn_few(const AttnArgs &a, char *lds, int p, in
                          pack_bf16x2(pr[6], pr[7])};
         pf[n] = __builtin_bit_cast(bf16x8, w);
       }
-      if (masked) {  // hidden tokens' values that are no numbers
+      if (masked) {  // hidden tokens' values that are no numbers (those of missing pages are zeros)
         u32x4 *w = reinterpret_cast<u32x4 *>(lds + wave * 2 * kStages * kTileB + buf * 2 * kTileB + kTileB) + lane;
         bool any = false;
 #pragma unroll
         for (int j = 0; j < 2 * kLoads; ++j) any |= attn_odd<kFp8>(w[64 * j]);
-        if (__ballot(any) != 0) {
+        if (__ballot(any) != 0 && !((t0 >= all_lo) & (t0 + 32 <= all_hi))) {
 #pragma unroll
           for (int j = 0; j < 2 * kLoads; ++j) w[64 * j] = attn_without_odd<kFp8>(w[64 * j]);
           odd = true;
@@ -358,7 +358,7 @@ __device__ __forceinline__ void attn_few(const AttnArgs &a, char *lds, int p, in
       __syncthreads();
     }
     if ((s_odd[0] | s_odd[1] | s_odd[2] | s_odd[3]) != 0)
-      attn_put_odd<D, kFp8>(a, sq, b, h, 0, rows, ga * kGran, tok_end, [&](int r, int d, float sum) {
+      attn_put_odd<D, kFp8, 32>(a, sq, b, h, 0, rows, ga * kGran, tok_end, all_lo, all_hi, [&](int r, int d, float sum) {
         if (whole)
           attn_put_out<D>(a, sq, h, r, d, sum);
         else

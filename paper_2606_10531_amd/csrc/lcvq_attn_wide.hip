@@ -352,7 +352,7 @@ __device__ __forceinline__ void attn_wide(const AttnArgs &a, char *lds, int bloc
   __syncthreads();
   if ((flags[0] | flags[1] | flags[2] | flags[3]) != 0) {
     float *part = a.part_wide + (((int64_t)item * a.Hkv + h) * splits + split) * wide_part_floats<D>();
-    attn_put_odd<D, kFp8>(a, sq, b, h, r0, r1, tok0, tok0 + tiles * kWideTok, [&](int r, int d, float sum) {
+    attn_put_odd<D, kFp8, kWideTok>(a, sq, b, h, r0, r1, tok0, tok0 + tiles * kWideTok, blk_lo, blk_hi, [&](int r, int d, float sum) {
       if (splits == 1)
         attn_put_out<D>(a, sq, h, r, d, sum);
       else

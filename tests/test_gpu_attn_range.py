@@ -104,3 +104,33 @@ def test_scale_bytes_that_the_format_has_not(lc, keys, seqs, window, back, byte)
     out[[i for i in range(n) if i not in blind]] = clean[0][[i for i in range(n) if i not in blind]]
     lse[[i for i in range(n) if i not in blind]] = clean[1][[i for i in range(n) if i not in blind]]
     c.check(out, lse, window=window)
+
+
+@pytest.mark.parametrize("fp8", [True, False])
+@pytest.mark.parametrize("new,length,window", [(512, 8192, 0), (512, 8192, 4096), (6, 8192, 0), (1, 8192, 4096)])
+def test_a_value_that_is_no_number_costs_little(lc, new, length, window, fp8):
+    """One NaN, or nothing but NaN on the last page, beside none: within ten times and half a millisecond."""
+    import torch
+    c = attn.Case([(new, length)], 8, 2, 128, 64, fp8, seed=34, stale="")
+    table, lens, starts = c.dev(c.table), c.dev([length]), c.dev(c.starts)
+
+    def ms():
+        times = []
+        for _ in range(4):
+            a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            a.record()
+            lc.attn_paged(c.q, c.data, table, lens, starts, c.scales, window=window)
+            b.record()
+            torch.cuda.synchronize()
+            times.append(a.elapsed_time(b))
+        return min(times)
+    plain = ms()
+    t = length - 2
+    c.data[1, c.table[0, t // 64], 0, t % 64, 5] = 255 if fp8 else float("nan")
+    one = ms()
+    c.data[1, c.table[0, (length - 1) // 64]] = 255 if fp8 else float("nan")
+    if window:
+        t = length - new - window + 1
+        c.data[1, c.table[0, t // 64]] = 255 if fp8 else float("nan")
+    many = ms()
+    assert max(one, many) <= 10 * plain + 0.5, (plain, one, many)
