@@ -413,6 +413,12 @@ def _arg(t, name, shape, dtype, device) -> int:
     return _dev(t, name)
 
 
+def _fits(x: int, name: str) -> None:
+    """For numbers of the caller's that the library takes in 32 bits (ctypes would cut them off)."""
+    if not -0x80000000 <= x < 0x80000000:
+        raise ValueError(f"{name}={x} does not fit 32 bits")
+
+
 def _cache(data, scales):
     """(format, pages, Hkv, page_size, D) and the four device pointers of a cache."""
     _check(data, "data", dtype=(torch.uint8, torch.bfloat16))
@@ -481,6 +487,8 @@ def kv_read(data: torch.Tensor, slots: torch.Tensor, scales: torch.Tensor | None
 
 def attn_workspace_bytes(T: int, B: int, Hq: int, Hkv: int, D: int, max_q: int) -> int:
     """Workspace of attn_paged for calls of at most T rows, B sequences and max_q new tokens each."""
+    for x, name in ((B, "B"), (Hq, "Hq"), (Hkv, "Hkv"), (D, "D"), (max_q, "max_q")):
+        _fits(x, name)
     return int(_lib.load().lcvq_attn_workspace_bytes(T, B, Hq, Hkv, D, max_q))
 
 
@@ -500,6 +508,11 @@ def attn_paged(q: torch.Tensor, data: torch.Tensor, table: torch.Tensor, kv_lens
     Returns (out, lse): T x query heads x head_dim bf16, and the log-sum-exp of the scaled
     scores, T x query heads fp32, or None unless need_lse or lse.  A row that sees nothing
     gives 0 and -inf."""
+    _fits(window, "window")
+    B, width = _check_2d(table, "table")
+    _fits(B, "sequences")
+    if max_q is not None:
+        _fits(max_q, "max_q")
     fmt, pages, H, page, D, ptr = _cache(data, scales)
     _check(q, "q", dtype=torch.bfloat16)
     if q.dim() != 3:
@@ -508,7 +521,6 @@ def attn_paged(q: torch.Tensor, data: torch.Tensor, table: torch.Tensor, kv_lens
     qp, qt, qh = _heads_view(q, "q", Hq, D, torch.bfloat16, dev)
     if H == 0 or Hq % H != 0 or Hq == 0:
         raise ValueError(f"{Hq} query heads on {H} cached heads")
-    B, width = _check_2d(table, "table")
     tp = _arg(table, "table", table.shape, torch.int32, dev)
     lp = _arg(kv_lens, "kv_lens", (B,), torch.int32, dev)
     sp = _arg(q_starts, "q_starts", (B + 1,), torch.int32, dev)
@@ -546,6 +558,7 @@ def linear_fwd_int4(packed: torch.Tensor, scales: torch.Tensor, X: torch.Tensor,
     of 128 columns, or both n/group x m, which large layers read up to 13 % faster.  The shape
     tells which; where m is n/group, by_group has to.  X is N x n bf16.  For few tokens: the
     weights are read once per 16."""
+    _fits(group, "group")
     m, n2 = _check_2d(packed, "packed")
     n = 2 * n2
     N, dev = _check_2d(X, "X")[0], X.device
