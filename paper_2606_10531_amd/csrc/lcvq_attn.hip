@@ -14,7 +14,8 @@
 //
 // 8-bit entries: the codes go to the matrix core as bf16 without their scale (exact); K's
 // scale multiplies the scores of its token, V's the probabilities, before they are
-// rounded to bf16 (a power of two, so the rounding is the same as without it).
+// rounded to bf16 (a power of two, so the rounding is the same as without it but for entries of
+// scales near 2^-117, whose small probabilities go below the least normal number).
 // Probabilities in bf16 cost 2^-9 relative each, as the output's own rounding does; their
 // sum is taken from the unrounded values.
 //
@@ -29,8 +30,9 @@
 // in flight while the current one is multiplied: no barrier in the loop.
 //
 // Bound: HBM, the visible entries once, and for a few hundred tokens the latency of a chain of
-// loads.  64 sequences of up to 8000 (620 MB), 64 heads of 128 on 8, e4m3: 118 us, 5.2 TB/s, the
-// rate of a large copy; one of 130001 54 us, 5 TB/s; one of 333, 32 heads, bf16: 7 us.
+// loads.  64 heads of 128 on 8: 64 sequences of up to 8000 in e4m3 (620 MB) 120 us, 5.2 TB/s, the rate
+// of a large copy; one of 130001 53 us, 5 TB/s; 16 of 8000 in bf16 (524 MB) 95 us, 5.5 TB/s; one of
+// 50000 in bf16 (205 MB) 40 us, 5.1 TB/s.  One of 333, 32 heads, bf16: 7 us.
 #include <algorithm>
 
 #include "lcvq_attn_few.hpp"
@@ -88,7 +90,8 @@ static hipError_t few(const AttnArgs &a, hipStream_t st) {
     return hipGetLastError();
   }
   // (one block to a compute unit where the registers or LDS hold no second one: 6 tokens of two
-  // sequences of 24000, 32 heads of 128 on 4, 46 -> 36 us)
+  // sequences of 24000, 32 heads of 128 on 4, e4m3: 46 -> 36 us a call.  Its kernel takes 27 us for
+  // the 50 MB and 30 for the 98 of bf16: four waves to a compute unit keep few loads in flight.)
   constexpr int64_t kAtOnce = (NB == 4 && D == 128) || attn_few_lds<D, kFp8, NB>() > 80 * 1024 ? 256 : kAttnFewBlocks;
   k_attn_few<D, kFp8, NB, false><<<(unsigned)std::min(attn_few_blocks(a), kAtOnce), 256, 0, st>>>(a);
   return join<D, NB>(a, st);

@@ -373,7 +373,7 @@ __device__ __forceinline__ void attn_few(const AttnArgs &a, char *lds, int p, in
 
 // ---- joining the pieces of a unit: their sums, maxima and sums of exponentials.
 // kShare groups of threads take the same rows of different pieces and add up in LDS, so that
-// 27 pieces (the most of a chunk's) are 7 rounds of loads.
+// 27 pieces are 7 rounds of loads.
 template <int D, int kShare>
 __host__ __device__ __forceinline__ constexpr int attn_join_rows() {  // rows of a block
   return 256 / (D / 4 * kShare);

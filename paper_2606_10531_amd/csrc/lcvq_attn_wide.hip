@@ -5,7 +5,7 @@
 // head; a block takes a unit, or one of `splits` parts of its visible tokens (wide_plan).  Its
 // four waves have 32 rows each and share tiles of 64 tokens in LDS as bf16, K and V in two
 // buffers each: 64 KiB for D = 128, so that two blocks stand on a compute unit, and one
-// multiplies while the other is at its softmax.  (One block of 256 rows with the softmax of a
+// can multiply while the other is at its softmax.  (One block of 256 rows with the softmax of a
 // tile woven between the products of the next takes 9 % longer at 512 tokens over 8192; one of
 // 512 threads and 256 rows 5 % less there, but 4 % more on prompts and 50 % on mixed batches.)
 //
@@ -14,19 +14,22 @@
 // the way, once per block, and with direct loads in flight the compiler waits for all of them
 // before each transposing read.  The stores lie between the second product's instructions.
 //
-// Bound: the vector units and the matrix cores.  A wave's 32 rows and 64 tokens are 64
-// instructions of 8.4 ns (the rate that the chip holds) at D = 128 and 32 exponentials per
-// lane with as many multiplications, sums, maxima and conversions.  512 tokens over 8192, 64
-// heads of 128 on 8, e4m3: 130 us and 9 for the join, 1.09 PFLOP/s while it multiplies; 512
-// over 8192, 32 heads of 64: 56 and 6 us, 1.3 PFLOP/s.  Three blocks of D = 64 on a compute
-// unit (168 registers) are no faster than two.
+// Bound: the vector units and the matrix cores, which overlap in small part.  A wave's 32 rows
+// and 64 tokens are 64 instructions of 8.4 ns (the rate that the chip holds) at D = 128 and 32
+// exponentials per lane with as many multiplications, sums, maxima and conversions.  512 tokens
+// over 8192 in e4m3, of whose cycles the matrix cores are busy in 0.40 and the vector units in 0.46
+// at 64 heads of 128 on 8 (133 GFLOP): 128 us once the clock has settled (150 the first dozen calls)
+// and 9 for the join, 1.04 PFLOP/s; 0.24 and 0.45 at 32 heads of 64 (33 GFLOP, but half as many
+// exponentials): 50 and 5 us, 0.66 PFLOP/s.  Three blocks of D = 64 on a compute unit (168
+// registers) are no faster than two.
 //
 // The running maximum follows only when a row's has grown by 8 in log2 units, so that
 // probabilities reach at most 2^8 and the rescaling branch is rare.  (Under the true maximum the
 // largest probability is 1, which bf16 holds; under a lagging one it is rounded like the others.)
 //
 // Blocks of one cached head follow one another every Hkv blocks, so that with 8 (16, ..)
-// heads an XCD's L2 holds its own head's entries; long units come first.
+// heads an XCD's L2 holds its own head's entries.  The sequences go from last to first, and of each
+// the last rows, which see most, come first: a long sequence in front begins late.
 #include <algorithm>
 #include <type_traits>
 #include <utility>
@@ -386,7 +389,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_mixed(AttnArgs a, int few, int 
     attn_wide<D, kFp8>(a, lds, (int)blockIdx.x - few, splits);
 }
 
-// Joins the parts of the units' tokens; the first `few` blocks those of the sequences with few
+// Joins the parts of the units' tokens (up to 64); the first `few` blocks those of the sequences with few
 // rows (NB 0: none).  kShare 4 for more than four parts (27 parts of 140 tokens over 7000, two
 // cached heads: 17 -> 5.6 us), else 1 (two parts of 512 tokens over 8192, 8 cached heads: 9.3 us,
 // 15.2 with four threads to a row, half of them idle).
@@ -422,7 +425,7 @@ struct WidePlan {
 // tokens as T has room for.  512 blocks run at once, and up to 256, one to a compute unit, take
 // 0.65 of the time (0.8 for D = 64 with nothing else to run, whose tiles are shorter than the
 // loads' way); a block begins and ends in 3 tiles' time, the join in another 3, and 512 parts
-// are written and read in 7 (5).  (900 tokens over 4096, 64 heads on 8: 456 units whole 131 us, in two
+// are written and read in 7 (5).  Blocks for single tokens beside them are not counted.  (900 tokens over 4096, 64 heads on 8: 456 units whole 131 us, in two
 // parts 152.  1500 over 8000, 32 heads of 64: 376 units whole 152 us, in two parts 145.)
 static WidePlan wide_plan(const AttnArgs &a, int D, bool alone) {
   const double one = D == 64 && alone ? 0.8 : 0.65, parts = D == 64 ? 5.0 : 7.0;

@@ -25,10 +25,10 @@
 // 28672 in groups of 64 at 16 tokens 39.8 / 36.4; up to 11008 columns and rows no difference.
 //
 // Bound: HBM, the codes once (0.5 byte per weight, and 2 or 4 bytes per group); at 16 tokens
-// also X from the L2, as many bytes as the codes of 64 rows.  28672 x 8192 with zero points, one
-// token: 28 us, 4.5 TB/s; 8192 x 28672 in groups of 64, 16 tokens: 32 us, 3.9 TB/s, and 4 for the
-// spans; 4096 x 4096, one token: 5 us, of which the codes at a copy's rate are 1.7 and the launch
-// the most.
+// also X from the L2, as many bytes as the codes of 64 rows.  28672 x 8192 with zero points by row, one
+// token: 35 us, 3.6 TB/s; 8192 x 28672 in groups of 64 by row, 16 tokens: 39 us, 3.2 TB/s, and 5 for
+// the spans; 4096 x 4096, one token: 5 us, of which the codes at a copy's rate are 1.7 and the
+// launch the most.
 #include <algorithm>
 
 #include "lcvq_mfma.hpp"
@@ -266,13 +266,18 @@ __global__ __launch_bounds__(256) void k_int4_sum(const float *__restrict__ part
 // those rounds full, MR at most 3 up to four tokens and 8 above, where a block's X counts
 // (28672 x 8192 at 16 tokens, 7 row blocks and four waves 33 us a call, 2 and eight 41); but 2
 // where four tokens or fewer meet more than 16384 rows (28672 x 8192 with zero points at one
-// token: 3 row blocks 28.9 us a call, 2 27.6, 1 28.4).
+// token: 3 row blocks 28.9 us a call, 2 27.6, 1 28.4.  Graphs of calls, 3 / 2 / 1 row blocks, by
+// group: 32000 x 4096 in groups of 32 30.2 / 23.5 / 25.5, 20000 x 8192 in groups of 64 23.9 / 23.6 /
+// 23.2, 17000 x 4096 12.8 / 13.1 / 12.7, 65536 x 2048 23.0 / 23.5 / 28.0, 128256 x 4096 55.8 / 58.9 /
+// 65.4; by row 41.5 / 35.1 / 34.0 for the first and 30.1 / 23.9 / 24.7 for the second).
 //
 // K is split over blocks, whose sums a second launch adds,
 //  - where there are fewer than 128 blocks of 16 rows, to fill the chip;
 //  - above four tokens where up to 8192 rows meet 128 steps or more: 64 rows a block read a
 //    quarter of the X that 16 do (8192 x 28672 at 16 tokens: 32 rows 36.1 us a call, 64 rows
-//    and two spans 33.8).
+//    and two spans 33.8.  Graphs of calls, whole K in the best of 16, 32 and 64 rows / 64 rows and
+//    spans, by group: 5120 x 27648 26.0 / 21.3, 4096 x 16384 15.1 / 14.3, 2048 x 16384 14.8 / 10.7, but
+//    6000 x 19968 in groups of 32 30.8 / 31.6 and, at the rule's end, 8192 x 16384 22.1 / 23.6).
 Int4Plan int4_plan(int64_t m, int64_t n, bool many, int most_mr) {
   Int4Plan p{};
   const int64_t rb = ceil_div(m, 16), rounds = ceil_div(rb, 256 * most_mr);

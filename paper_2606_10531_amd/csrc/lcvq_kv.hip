@@ -10,9 +10,10 @@
 // token, eight entries each (16 bytes of bf16), and share amax by lane moves.  A block takes
 // 16 (D = 128) or 32 tokens of four heads of K or V: the tokens that follow one another in a page
 // make whole lines of codes and runs of scale bytes, the four heads a run of 1 KiB (512
-// bytes) of the dense side.  4999 tokens of 32 heads of 128, e4m3 (246 MB both ways): write 28 us,
-// read 24, 4.7 TB/s; 100000 tokens of 8 heads read 116 us, 5.3 TB/s, a large copy's rate.  One
-// token: 4 us, its launch.
+// bytes) of the dense side.  4999 tokens of 32 heads of 128, e4m3 (246 MB both ways): write 29 us,
+// read 22, 4.2 and 5.7 TB/s; in bf16 (328 MB) 35 and 30; from fp32 and to fp32 (410 MB) 48 and
+// 35.  100000 tokens of 8 heads read 119 us, 5.2 TB/s, a large copy's rate; 50000 in bf16 (410 MB) 81.
+// One token: 3 us, its launch.
 #include "lcvq_prep.hpp"
 #include "lcvq_serve.hpp"
 
