@@ -16,7 +16,7 @@
 // scale multiplies the scores of its token, V's the probabilities, before they are
 // rounded to bf16 (a power of two, so the rounding is the same as without it but for entries of
 // scales near 2^-117, whose small probabilities go below the least normal number).
-// Probabilities in bf16 cost 2^-9 relative each, as the output's own rounding does; their
+// Probabilities in bf16 cost up to 2^-8 relative each, as the output's own rounding does; their
 // sum is taken from the unrounded values.
 //
 // Work: a unit is (sequence, cached head); its visible tokens are granules of 128, 32 per

@@ -18,8 +18,8 @@
 // and 64 tokens are 64 instructions of 8.4 ns (the rate that the chip holds) at D = 128 and 32
 // exponentials per lane with as many multiplications, sums, maxima and conversions.  512 tokens
 // over 8192 in e4m3, of whose cycles the matrix cores are busy in 0.40 and the vector units in 0.46
-// at 64 heads of 128 on 8 (133 GFLOP): 128 us once the clock has settled (150 the first dozen calls)
-// and 9 for the join, 1.04 PFLOP/s; 0.24 and 0.45 at 32 heads of 64 (33 GFLOP, but half as many
+// at 64 heads of 128 on 8 (133 GFLOP): 128 to 134 us once the clock has settled (two cards; 150 the
+// first dozen calls) and 9 for the join, 1.0 PFLOP/s; 0.24 and 0.45 at 32 heads of 64 (33 GFLOP, but half as many
 // exponentials): 50 and 5 us, 0.66 PFLOP/s.  Three blocks of D = 64 on a compute unit (168
 // registers) are no faster than two.
 //
